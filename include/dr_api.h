@@ -496,14 +496,16 @@ size_t dr_qk_norm_rope_workspace_size(int64_t rows, int64_t D);
  *   q [rows][ldq] of Hq heads; k, v [rows][ldk], [rows][ldv] of Hkv heads, Hkv
  *             dividing Hq; D in {64, 128}.
  *   N, T      sequences, and the most tokens of one.
- *   off       device int32 [N + 1], off[0] = 0: sequence i holds rows off[i] ..
- *             off[i + 1] - 1 (packed).  NULL: rows i T .. i T + T - 1 (padded;
- *             rows must be N * T).
+ *   off       device int32 [N + 1], off[0] = 0, ascending: sequence i holds rows
+ *             off[i] .. off[i + 1] - 1 (packed).  NULL: rows i T .. i T + T - 1
+ *             (padded; rows must be N * T).
  *   len       device int32 [N] or NULL: only the first len[i] rows of sequence
  *             i's slot are tokens.  The others are padding: never read (they
  *             may hold any bits, NaN included), and o and lse are zero there, as
- *             they are in rows after the last slot.  Values of off and len out
- *             of range are clamped; a sequence has at most T tokens.
+ *             they are in rows after the last slot.  Values of off and len below
+ *             0 or above the rows are clamped; a sequence has at most T tokens.
+ *             (Offsets that descend reach no memory outside the tensors either,
+ *             but which rows are written, and with what, is then undefined.)
  *   dtype     DR_BF16 (DR_F32: DR_ERR_UNSUPPORTED).
  *   o [rows][ldo] of Hq heads; lse fp32 [Hq][rows].
  * Arithmetic: bf16 MFMA with fp32 accumulation; scores and softmax statistics

@@ -165,6 +165,12 @@ struct Seq {
   long long first, end;
   int len;
 };
+// A packed slot's ends, clamped into the rows: the slots of ascending offsets then take
+// every row at most once, whatever their values (what the grid of listed places rests on).
+__device__ __forceinline__ void clamp_slot(const Batch& b, long long& first, long long& next) {
+  first = first < 0 ? 0 : (first > b.rows ? b.rows : first);
+  next = next < first ? first : (next > b.rows ? b.rows : next);
+}
 // Values outside their range are clamped: no row outside [0, rows) is touched.  (i
 // is uniform; the constant address space makes these scalar loads, which do not
 // queue behind the vector loads of the waves around.)
@@ -177,8 +183,7 @@ __device__ __forceinline__ Seq sequence(const Batch& b, int i) {
   if (b.off) {
     s.first = ((Ints)b.off)[u];
     next = ((Ints)b.off)[u + 1];
-    s.first = s.first < 0 ? 0 : (s.first > b.rows ? b.rows : s.first);
-    next = next < s.first ? s.first : (next > b.rows ? b.rows : next);
+    clamp_slot(b, s.first, next);
   } else {
     s.first = i * b.T;
     next = s.first + b.T;
@@ -235,8 +240,9 @@ __device__ __forceinline__ bool listed_place(const Grid& q, const Batch& b, int 
     const int i = lane + 64 * j;
     nt[j] = 0;
     if (i < b.N) {
-      long long n = (long long)b.off[i + 1] - b.off[i];
-      n = n < 0 ? 0 : (n > b.T ? b.T : n);
+      long long first = b.off[i], next = b.off[i + 1];
+      clamp_slot(b, first, next);
+      const long long n = next - first < b.T ? next - first : b.T;
       nt[j] = (int)((n + q.own - 1) / q.own);
       if (i == b.N - 1 && nt[j] == 0) nt[j] = 1;
     }

@@ -305,3 +305,24 @@ def test_no_rows_and_no_sequences():
     o, lse = api.attention(q, k, v, offsets=off, max_len=0)
     assert o.numel() == 0 and lse.numel() == 0
     assert all(t.numel() == 0 for t in api.attention_backward(g, q, k, v, o, lse, offsets=off, max_len=0))
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(2, 1), (66, 2)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_offsets_out_of_range(D, Hq, Hkv):
+    """Offsets below 0 and above the rows count as 0 and as the rows, whether the launch goes over all pairs of a sequence
+    and a tile (max_len 128) or workgroups look for their own (max_len 4096), with tiles of 32 rows (2 heads) and 128."""
+    rows = 128
+    q, k, v, g = make(rows, Hq, Hkv, D, True, 31)
+    given, clamped = [-9, 64, 100, 5000, 1 << 30], [0, 64, 100, 128, 128]
+    off = torch.tensor(given, dtype=torch.int32, device=DEV)
+    spans = ref.spans_of(clamped, None, 4, 0)
+    want = ref.attention(q, k, v, spans, D ** -0.5, g)
+    for most in (128, 4096):
+        o, lse = torch.full_like(q, 7.0), torch.full((Hq, rows), 7.0, device=DEV)
+        grads = [torch.full_like(t, 7.0) for t in (q, k, v)]
+        ws = torch.full((api.dr_attention_workspace_size(rows, Hq, Hkv, D),), 255, dtype=torch.uint8, device=DEV)
+        api.dr_attention(q, k, v, off, None, most, None, o, lse)
+        api.dr_attention_backward(g, q, k, v, o, lse, off, None, most, None, *grads, workspace=ws)
+        assert rel(o, want[0]) <= TOL_O and float((ref.d64(lse) - want[1]).abs().max()) <= TOL_LSE
+        assert rel(grads[0], want[2]) <= TOL_DQK and rel(grads[1], want[3]) <= TOL_DQK and rel(grads[2], want[4]) <= TOL_DV

@@ -294,8 +294,9 @@ __global__ __launch_bounds__(kThreads, 1) void attn_few_kernel(FwdArgs a) {
   for (int i = 1; i < kWaves; ++i) top = fmaxf(top, stat[i * 64 + (lane & 31)]);
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) {
-    const float mi = stat[i * 64 + (lane & 31)];
-    if (mi != -INFINITY) total += stat[i * 64 + 32 + (lane & 31)] * __builtin_amdgcn_exp2f((mi - top) * c);
+    // (a wave without a step has m = -inf and sum 0; one whose scores are all NaN has sum NaN)
+    const float mi = stat[i * 64 + (lane & 31)], scale = mi == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mi - top) * c);
+    total = fmaf(stat[i * 64 + 32 + (lane & 31)], scale, total);
   }
   const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * c) / total;
   if (w == 0 && h == 0 && row < s.len) a.lse[(long long)head * a.b.rows + s.first + row] = top * a.scale + __logf(total);

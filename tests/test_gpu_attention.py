@@ -326,3 +326,27 @@ def test_offsets_out_of_range(D, Hq, Hkv):
         api.dr_attention_backward(g, q, k, v, o, lse, off, None, most, None, *grads, workspace=ws)
         assert rel(o, want[0]) <= TOL_O and float((ref.d64(lse) - want[1]).abs().max()) <= TOL_LSE
         assert rel(grads[0], want[2]) <= TOL_DQK and rel(grads[1], want[3]) <= TOL_DQK and rel(grads[2], want[4]) <= TOL_DV
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(2, 1), (32, 2)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_nan_reaches_the_statistics_it_belongs_to(D, Hq, Hkv):
+    """A NaN in a key makes o and lse NaN in that key's row and every later one of its sequence, a NaN in a query in its
+    own row, with tiles of 32 rows (2 heads) and 128; lse keeps its bits elsewhere."""
+    lens, at = [200, 129, 65, 200, 33, 1], [0, 32, 64, 96, 31, 0]
+    off = [0]
+    for n in lens:
+        off.append(off[-1] + n)
+    rows = off[-1]
+    where = dict(offsets=torch.tensor(off, dtype=torch.int32, device=DEV), max_len=max(lens))
+    q, k, v, _ = make(rows, Hq, Hkv, D, False, 32)
+    _, base = api.attention(q, k, v, **where)
+    for which in (k, q):
+        bad = torch.zeros(rows, dtype=torch.bool, device=DEV)
+        x = which.clone()
+        for a, b, i in zip(off, off[1:], at):
+            x[a + i, :, 5] = float("nan")
+            bad[a + i:b if which is k else a + i + 1] = True
+        o, lse = api.attention(x if which is q else q, x if which is k else k, v, **where)
+        assert bool(torch.isnan(lse[:, bad]).all()) and bool(torch.isnan(o[bad].float()).all())
+        assert torch.equal(lse[:, ~bad], base[:, ~bad])

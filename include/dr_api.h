@@ -545,8 +545,9 @@ size_t dr_attention_workspace_size(int64_t rows, int Hq, int Hkv, int64_t D);
  *   loss, lse fp32 [M].
  *   workspace at least dr_cross_entropy_workspace_size(M, V, D, 0) bytes.
  * Arithmetic: bf16 MFMA with fp32 accumulation, everything else in fp32.
- * Requirements (else DR_ERR_ARG): D, ldh, ldw multiples of 8, ld >= D; tensors
- * and workspace 16-byte aligned.  M < 2^24, D <= 65536, and at most 2^24 - 1024
+ * Requirements (else DR_ERR_ARG): D, ldh, ldw multiples of 8, ld >= D, ldw at
+ * most 2^22, the other leading dimensions (those of the gradients among them)
+ * 2^32; tensors and workspace 16-byte aligned.  M < 2^24, D <= 65536, and at most 2^24 - 1024
  * workgroups in a launch (else DR_ERR_UNSUPPORTED): ceil(V / 64) * ceil(D / 256),
  * and ceil(M / 256) * ceil(V / 256), or ceil(M / 64) * ceil(V / 256) with D < 256.
  * ------------------------------------------------------------------------- */

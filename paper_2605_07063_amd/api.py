@@ -597,7 +597,7 @@ def _matrix(t, name, rows=None, cols=None):
         raise ValueError(f"{name} must be a matrix with unit column stride")
     if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
         raise ValueError(f"{name} must be [{rows}, {cols}]")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]      # (the stride of a single row says nothing)
 
 
 def _xent_args(h, weight, target):

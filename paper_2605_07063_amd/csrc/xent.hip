@@ -1027,7 +1027,12 @@ bool sizes_supported(int64_t M, int64_t V, int64_t D) {
   const int64_t logits = (logit_strips(M, V, D) ? strips_of(M) : tiles_of(M)) * tiles_of(V);
   return logits <= most && strips_of(V) * tiles_of(D) <= most;
 }
-bool good(const void* p, int64_t ld, int64_t D) { return p && aligned16(p) && ld >= D && ld % 8 == 0 && ld <= (1 << 22); }
+// W's rows are at most 2^22 values apart: a panel's 256 rows take 32-bit offsets.  Rows of
+// the others are addressed one by one, in 64 bits.
+constexpr int64_t kMaxLdw = 1 << 22, kMaxLd = (int64_t)1 << 32;
+bool good(const void* p, int64_t ld, int64_t D, int64_t most = kMaxLd) {
+  return p && aligned16(p) && ld >= D && ld % 8 == 0 && ld <= most;
+}
 
 }  // namespace
 }  // namespace xent
@@ -1047,7 +1052,7 @@ extern "C" dr_status dr_cross_entropy(const void* h, int64_t ldh, const void* W,
   if (dtype != DR_BF16) return dtype == DR_F32 ? DR_ERR_UNSUPPORTED : DR_ERR_DTYPE;
   if (!sizes_ok(M, V, D)) return DR_ERR_ARG;
   if (M == 0) return DR_OK;
-  if (!good(h, ldh, D) || !good(W, ldw, D) || !target || !loss || !lse) return DR_ERR_ARG;
+  if (!good(h, ldh, D) || !good(W, ldw, D, kMaxLdw) || !target || !loss || !lse) return DR_ERR_ARG;
   if (!sizes_supported(M, V, D)) return DR_ERR_UNSUPPORTED;
   const Layout l = layout(M, V, D, false);
   if (!workspace || ws_bytes < l.end) return DR_ERR_WORKSPACE;
@@ -1098,7 +1103,7 @@ extern "C" dr_status dr_cross_entropy_backward(const void* h, int64_t ldh, const
   if (dtype != DR_BF16) return dtype == DR_F32 ? DR_ERR_UNSUPPORTED : DR_ERR_DTYPE;
   if (!sizes_ok(M, V, D)) return DR_ERR_ARG;
   if ((dh && !good(dh, lddh, D)) || (dW && !good(dW, lddw, D))) return DR_ERR_ARG;
-  if (M > 0 && (!good(h, ldh, D) || !good(W, ldw, D) || !target || !lse || !g)) return DR_ERR_ARG;
+  if (M > 0 && (!good(h, ldh, D) || !good(W, ldw, D, kMaxLdw) || !target || !lse || !g)) return DR_ERR_ARG;
   if (!sizes_supported(M, V, D)) return DR_ERR_UNSUPPORTED;
   if (!dh && !dW) return DR_OK;
   if (M == 0 && !dW) return DR_OK;

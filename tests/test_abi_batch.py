@@ -132,3 +132,14 @@ def test_cross_entropy_grid(lib, back):
         d = dict(ldh=D, ldw=D, lddh=D, lddw=D, M=M, V=V, D=D)
         assert (xent(lib, back, ws=None, **d) == (DR_ERR_WORKSPACE if ok else DR_ERR_UNSUPPORTED)), d
         assert (lib.dr_cross_entropy_workspace_size(M, V, D, int(back)) > 0) == ok, d
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_cross_entropy_leading_dimensions(lib, back):
+    # h, dh and dW may have any (one token of every long example: T D between rows); W's rows, of which a tile spans 256
+    # at 32-bit offsets, are at most 2^22 apart
+    for ld, ok in [(1 << 22, True), ((1 << 22) + 8, False)]:
+        assert xent(lib, back, ldw=ld, ws=None) == (DR_ERR_WORKSPACE if ok else DR_ERR_ARG)
+    for ld, ok in [(1 << 24, True), (1 << 32, True), ((1 << 32) + 8, False)]:
+        for name in ("ldh", "lddh", "lddw") if back else ("ldh",):
+            assert xent(lib, back, ws=None, **{name: ld}) == (DR_ERR_WORKSPACE if ok else DR_ERR_ARG), (name, ld)

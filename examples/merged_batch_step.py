@@ -77,7 +77,7 @@ def forward_backward(w, x, lens, target):
     flat = x.view(N * T, d)
     qkv = (flat @ w["qkv"].t()).view(N, T, Hq + 2 * Hkv, D)
     q, k, v = qkv.split([Hq, Hkv, Hkv], dim=2)                      # views: the kernels take the row stride
-    qr, kr = api.qk_norm_rope(q, k, w["table"], w["wq"], w["wk"])   # a row's position is its place in the example
+    qr, kr = api.qk_norm_rope(q, k, w["table"], w["wq"], w["wk"], lengths=lens)   # positions: places in the example
     o, lse = api.attention(qr, kr, v, lengths=lens)
     y = o.view(N * T, Hq * D) @ w["o"].t() + flat
     t = target.reshape(-1)
@@ -88,7 +88,7 @@ def forward_backward(w, x, lens, target):
     dy, _ = api.cross_entropy_backward(y, w["head"], t, z, g, need_dweight=False)
     do = (dy @ w["o"]).view(N, T, Hq, D)
     dqr, dkr, dv = api.attention_backward(do, qr, kr, v, o, lse, lengths=lens)
-    dq, dk, _, _ = api.qk_norm_rope_backward(dqr, dkr, q, k, w["table"], w["wq"], w["wk"])
+    dq, dk, _, _ = api.qk_norm_rope_backward(dqr, dkr, q, k, w["table"], w["wq"], w["wk"], lengths=lens)
     pairs = [(x, dq.view(N, T, -1)), (x, dk.view(N, T, -1)), (x, dv.view(N, T, -1)),
              (o.view(N, T, -1), dy.view(N, T, d))]
     return loss.view(N, T), pairs

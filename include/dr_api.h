@@ -488,6 +488,25 @@ dr_status dr_qk_norm_rope_backward(const void* gq, int64_t ldgq, const void* gk,
                                    float* dwq, float* dwk, void* workspace, size_t ws_bytes, void* stream);
 size_t dr_qk_norm_rope_workspace_size(int64_t rows, int64_t D);
 
+/* dr_qk_norm_rope_batch, dr_qk_norm_rope_batch_backward -- the same over a batch
+ * of sequences with padding: N, T, off and len as in dr_attention (below), pos
+ * NULL: a row's place in its sequence.  Rows that hold no token are never read
+ * (q, k, gq, gk may hold any bits there, NaN included), their outputs are zero,
+ * and they add nothing to dwq and dwk.  Without off and len every row is a token,
+ * as in dr_qk_norm_rope (where padding is read like any other row). */
+dr_status dr_qk_norm_rope_batch(const void* q, int64_t ldq, const void* k, int64_t ldk, int64_t rows, int64_t N,
+                                int64_t T, const int32_t* off, const int32_t* len, int Hq, int Hkv, int64_t D,
+                                dr_dtype dtype, const float* wq, const float* wk, float eps, const float* table,
+                                int64_t table_rows, const int32_t* pos, dr_rope_pairing pairing, void* q_out,
+                                int64_t ldqo, void* k_out, int64_t ldko, void* stream);
+dr_status dr_qk_norm_rope_batch_backward(const void* gq, int64_t ldgq, const void* gk, int64_t ldgk, const void* q,
+                                         int64_t ldq, const void* k, int64_t ldk, int64_t rows, int64_t N, int64_t T,
+                                         const int32_t* off, const int32_t* len, int Hq, int Hkv, int64_t D,
+                                         dr_dtype dtype, const float* wq, const float* wk, float eps,
+                                         const float* table, int64_t table_rows, const int32_t* pos,
+                                         dr_rope_pairing pairing, void* dq, int64_t lddq, void* dk, int64_t lddk,
+                                         float* dwq, float* dwk, void* workspace, size_t ws_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------
  * dr_attention -- causal attention within each sequence of the batch:
  *   o_i = sum_{j <= i} softmax_j(scale q_i . k_j) v_j,

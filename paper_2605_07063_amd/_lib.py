@@ -74,6 +74,11 @@ SIGNATURES = {
     "dr_qk_norm_rope_backward": (c_int, [c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_i64, c_i64, c_int, c_int,
                                          c_i64, c_int, c_vp, c_vp, c_float, c_vp, c_i64, c_vp, c_int, c_vp, c_i64, c_vp,
                                          c_i64, c_vp, c_vp, c_vp, c_size, c_vp]),
+    "dr_qk_norm_rope_batch": (c_int, [c_vp, c_i64, c_vp, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, c_int, c_int, c_i64, c_int,
+                                      c_vp, c_vp, c_float, c_vp, c_i64, c_vp, c_int, c_vp, c_i64, c_vp, c_i64, c_vp]),
+    "dr_qk_norm_rope_batch_backward": (c_int, [c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_i64, c_i64, c_i64, c_vp,
+                                               c_vp, c_int, c_int, c_i64, c_int, c_vp, c_vp, c_float, c_vp, c_i64, c_vp,
+                                               c_int, c_vp, c_i64, c_vp, c_i64, c_vp, c_vp, c_vp, c_size, c_vp]),
     "dr_qk_norm_rope_workspace_size": (c_size, [c_i64, c_i64]),
     "dr_attention": (c_int, [c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, c_int, c_int, c_i64,
                              c_int, c_float, c_vp, c_i64, c_vp, c_vp]),

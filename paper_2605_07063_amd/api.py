@@ -453,7 +453,30 @@ def _like_heads(t, H, D, name, rows, dtype):
     return ld
 
 
-def _rope_args(q, k, table, wq, wk, pos):
+def _layout(q, rows, offsets, lengths, max_len):
+    """N, T of a batch whose rows q holds: packed by offsets [N + 1], or padded."""
+    if offsets is not None:
+        _dev(offsets, "offsets", torch.int32)
+        _contig(offsets, "offsets")
+        N = offsets.numel() - 1
+        if N < 0 or max_len is None:
+            raise ValueError("packed sequences need offsets [N + 1] and max_len")
+        T = int(max_len)
+    elif q.dim() == 4:
+        N, T = q.shape[0], q.shape[1]
+    elif max_len is not None and max_len > 0 and rows % max_len == 0:
+        N, T = rows // int(max_len), int(max_len)
+    else:
+        raise ValueError("rows of padded sequences need [N, T, H, D] or a max_len that divides them")
+    if lengths is not None:
+        _dev(lengths, "lengths", torch.int32)
+        _contig(lengths, "lengths")
+        if lengths.numel() != N:
+            raise ValueError(f"lengths must have {N} values")
+    return N, T
+
+
+def _rope_args(q, k, table, wq, wk, pos, offsets, lengths, max_len):
     if q.dtype not in _DTYPES:
         raise ValueError("q must be float32 or bfloat16")
     rows, ldq, Hq, D = _heads(q, "q")
@@ -477,35 +500,43 @@ def _rope_args(q, k, table, wq, wk, pos):
         _contig(pos, "pos")
         if pos.numel() != rows:
             raise ValueError(f"pos must have {rows} values")
-    T = q.shape[1] if q.dim() == 4 else rows
-    return rows, max(T, 1), ldq, ldk, Hq, Hkv, D
+    if offsets is not None or lengths is not None:
+        N, T = _layout(q, rows, offsets, lengths, max_len)
+    elif q.dim() == 4:
+        N, T = q.shape[0], q.shape[1]
+    else:
+        N, T = 1, rows
+    return rows, ldq, ldk, Hq, Hkv, D, N, T
 
 
-def _qk_norm_rope(args, q, k, table, wq, wk, eps, pos, pairs, qo, ldqo, ko, ldko, stream):
-    rows, T, ldq, ldk, Hq, Hkv, D = args
-    check("dr_qk_norm_rope", _lib.load().dr_qk_norm_rope(
-        q.data_ptr(), ldq, k.data_ptr(), ldk, rows, T, Hq, Hkv, D, _DTYPES[q.dtype], _ptr(wq), _ptr(wk), eps,
-        table.data_ptr(), table.shape[0], _ptr(pos), 1 if pairs else 0, qo.data_ptr(), ldqo, ko.data_ptr(), ldko,
-        _stream(stream)))
+def _qk_norm_rope(args, q, k, table, wq, wk, eps, pos, pairs, qo, ldqo, ko, ldko, stream, offsets, lengths):
+    rows, ldq, ldk, Hq, Hkv, D, N, T = args
+    check("dr_qk_norm_rope_batch", _lib.load().dr_qk_norm_rope_batch(
+        q.data_ptr(), ldq, k.data_ptr(), ldk, rows, N, T, _ptr(offsets), _ptr(lengths), Hq, Hkv, D, _DTYPES[q.dtype],
+        _ptr(wq), _ptr(wk), eps, table.data_ptr(), table.shape[0], _ptr(pos), 1 if pairs else 0, qo.data_ptr(), ldqo,
+        ko.data_ptr(), ldko, _stream(stream)))
 
 
-def dr_qk_norm_rope(q, k, table, wq, wk, eps, pos, pairs, q_out, k_out, stream=None):
-    """Per-head RMS norm (none when wq, wk are None) of q and k and the rotation by the rows' positions."""
-    args = _rope_args(q, k, table, wq, wk, pos)
-    rows, _, _, _, Hq, Hkv, D = args
+def dr_qk_norm_rope(q, k, table, wq, wk, eps, pos, pairs, q_out, k_out, stream=None, offsets=None, lengths=None,
+                    max_len=None):
+    """Per-head RMS norm (none when wq, wk are None) of q and k and the rotation by the rows' positions; with lengths or
+    offsets (as in dr_attention) padding is not read and comes out as zeros."""
+    args = _rope_args(q, k, table, wq, wk, pos, offsets, lengths, max_len)
+    rows, _, _, Hq, Hkv, D, _, _ = args
     ldqo = _like_heads(q_out, Hq, D, "q_out", rows, q.dtype)
     ldko = _like_heads(k_out, Hkv, D, "k_out", rows, q.dtype)
-    _qk_norm_rope(args, q, k, table, wq, wk, eps, pos, pairs, q_out, ldqo, k_out, ldko, stream)
+    _qk_norm_rope(args, q, k, table, wq, wk, eps, pos, pairs, q_out, ldqo, k_out, ldko, stream, offsets, lengths)
 
 
 def dr_qk_norm_rope_workspace_size(rows, D):
     return _lib.load().dr_qk_norm_rope_workspace_size(rows, D)
 
 
-def dr_qk_norm_rope_backward(gq, gk, q, k, table, wq, wk, eps, pos, pairs, dq, dk, dwq, dwk, workspace=None, stream=None):
+def dr_qk_norm_rope_backward(gq, gk, q, k, table, wq, wk, eps, pos, pairs, dq, dk, dwq, dwk, workspace=None, stream=None,
+                             offsets=None, lengths=None, max_len=None):
     """Gradients of dr_qk_norm_rope from those of its outputs; dwq, dwk are None without norms."""
     lib = _lib.load()
-    rows, T, ldq, ldk, Hq, Hkv, D = _rope_args(q, k, table, wq, wk, pos)
+    rows, ldq, ldk, Hq, Hkv, D, N, T = _rope_args(q, k, table, wq, wk, pos, offsets, lengths, max_len)
     lds = [_like_heads(t, H, D, nm, rows, q.dtype)
            for t, H, nm in ((gq, Hq, "gq"), (gk, Hkv, "gk"), (dq, Hq, "dq"), (dk, Hkv, "dk"))]
     ws, wsb = None, 0
@@ -516,10 +547,10 @@ def dr_qk_norm_rope_backward(gq, gk, q, k, table, wq, wk, eps, pos, pairs, dq, d
             if w.numel() != D:
                 raise ValueError(f"{nm} must have {D} values")
         ws, wsb = _workspace(lib.dr_qk_norm_rope_workspace_size(rows, D), q.device, workspace, stream)
-    check("dr_qk_norm_rope_backward", lib.dr_qk_norm_rope_backward(
-        _ptr(gq), lds[0], _ptr(gk), lds[1], _ptr(q), ldq, _ptr(k), ldk, rows, T, Hq, Hkv, D, _DTYPES[q.dtype], _ptr(wq),
-        _ptr(wk), float(eps), _ptr(table), table.shape[0], _ptr(pos), int(bool(pairs)), _ptr(dq), lds[2], _ptr(dk), lds[3],
-        _ptr(dwq), _ptr(dwk), _ptr(ws), wsb, _stream(stream)))
+    check("dr_qk_norm_rope_batch_backward", lib.dr_qk_norm_rope_batch_backward(
+        _ptr(gq), lds[0], _ptr(gk), lds[1], _ptr(q), ldq, _ptr(k), ldk, rows, N, T, _ptr(offsets), _ptr(lengths), Hq, Hkv, D,
+        _DTYPES[q.dtype], _ptr(wq), _ptr(wk), float(eps), _ptr(table), table.shape[0], _ptr(pos), int(bool(pairs)),
+        _ptr(dq), lds[2], _ptr(dk), lds[3], _ptr(dwq), _ptr(dwk), _ptr(ws), wsb, _stream(stream)))
 
 
 def _attention_args(q, k, v, offsets, lengths, max_len, scale):
@@ -528,24 +559,7 @@ def _attention_args(q, k, v, offsets, lengths, max_len, scale):
     ldv = _like_heads(v, Hkv, D, "v", rows, torch.bfloat16)
     if rk != rows or Dk != D:
         raise ValueError(f"k must have {rows} rows of heads of {D}")
-    if offsets is not None:
-        _dev(offsets, "offsets", torch.int32)
-        _contig(offsets, "offsets")
-        N = offsets.numel() - 1
-        if N < 0 or max_len is None:
-            raise ValueError("packed sequences need offsets [N + 1] and max_len")
-        T = int(max_len)
-    elif q.dim() == 4:
-        N, T = q.shape[0], q.shape[1]
-    elif max_len is not None and max_len > 0 and rows % max_len == 0:
-        N, T = rows // int(max_len), int(max_len)
-    else:
-        raise ValueError("rows of padded sequences need [N, T, H, D] or a max_len that divides them")
-    if lengths is not None:
-        _dev(lengths, "lengths", torch.int32)
-        _contig(lengths, "lengths")
-        if lengths.numel() != N:
-            raise ValueError(f"lengths must have {N} values")
+    N, T = _layout(q, rows, offsets, lengths, max_len)
     return rows, N, T, ldq, ldk, ldv, Hq, Hkv, D, float(D ** -0.5 if scale is None else scale)
 
 
@@ -806,24 +820,32 @@ def _contiguous_like(t):
     return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
-def qk_norm_rope(q, k, table, wq=None, wk=None, eps=1e-6, pos=None, pairs=False, stream=None):
+def qk_norm_rope(q, k, table, wq=None, wk=None, eps=1e-6, pos=None, pairs=False, stream=None, offsets=None, lengths=None,
+                 max_len=None):
     """Normed and rotated q and k (contiguous).  table [positions, D/2, 2]: cosines and sines; pos int32 per row, or
-    None: the row's place in its [N, T, H, D] example.  pairs: rotate (2i, 2i + 1) instead of (i, i + D/2)."""
-    args = _rope_args(q, k, table, wq, wk, pos)
+    None: the row's place in its [N, T, H, D] example.  pairs: rotate (2i, 2i + 1) instead of (i, i + D/2).
+
+    offsets, lengths, max_len as in `attention`: rows without a token are not read and come out as zeros, and pos None is
+    a row's place in its sequence.  Without them every row is a token, padding too."""
+    args = _rope_args(q, k, table, wq, wk, pos, offsets, lengths, max_len)
+    rows, _, _, Hq, Hkv, D, _, _ = args
     qo, ko = _contiguous_like(q), _contiguous_like(k)
     _keep(stream, qo, ko)
-    _qk_norm_rope(args, q, k, table, wq, wk, eps, pos, pairs, qo, args[4] * args[6], ko, args[5] * args[6], stream)
+    _qk_norm_rope(args, q, k, table, wq, wk, eps, pos, pairs, qo, Hq * D, ko, Hkv * D, stream, offsets, lengths)
     return qo, ko
 
 
-def qk_norm_rope_backward(gq, gk, q, k, table, wq=None, wk=None, eps=1e-6, pos=None, pairs=False, stream=None):
-    """dq, dk, dwq, dwk (the last two None without norm weights)."""
+def qk_norm_rope_backward(gq, gk, q, k, table, wq=None, wk=None, eps=1e-6, pos=None, pairs=False, stream=None, offsets=None,
+                          lengths=None, max_len=None):
+    """dq, dk, dwq, dwk (the last two None without norm weights).  With lengths or offsets padding is not read, gets zeros
+    and adds nothing to dwq and dwk; without them a NaN in a padding row's q makes dwq NaN even where its gq is 0."""
     dq, dk = _contiguous_like(q), _contiguous_like(k)
     dwq = dwk = None
     if wq is not None:
         dwq, dwk = torch.empty_like(wq), torch.empty_like(wk)
     _keep(stream, dq, dk, dwq, dwk)
-    dr_qk_norm_rope_backward(gq, gk, q, k, table, wq, wk, eps, pos, pairs, dq, dk, dwq, dwk, stream=stream)
+    dr_qk_norm_rope_backward(gq, gk, q, k, table, wq, wk, eps, pos, pairs, dq, dk, dwq, dwk, None, stream, offsets, lengths,
+                             max_len)
     return dq, dk, dwq, dwk
 
 

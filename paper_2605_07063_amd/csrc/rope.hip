@@ -16,7 +16,7 @@
 // one bf16 head) is read once per row and not once per head.  bf16, D = 128: 16384 rows
 // of 40 heads out of the fused projection, rotated only, 64 us (5.2 TB/s, where a copy
 // reaches 4.9); 36864 rows of 24 heads with norms 79 us, their gradients 134 us (680 MB).
-#include "common.h"
+#include "attn.h"   // the batch's rows
 
 namespace dr {
 namespace {
@@ -38,6 +38,9 @@ struct RopeArgs {
   float eps;
   int Hq, H;        // query heads, all heads
   float* partial;   // backward: [blocks][2][D]
+  bool batch;       // sequences with padding, or packed ones
+  attn::Batch b;
+  attn::Divisor perT;
 };
 
 template <bool BF16, int N>
@@ -104,11 +107,50 @@ __device__ __forceinline__ void turn(float (&a)[N], float (&b)[N], const float (
   }
 }
 
-// the lane's N angles at the row's position (clamped into the table)
-template <bool PAIRS, int N, int D>
-__device__ __forceinline__ void load_angles(const RopeArgs& a, long long row, int j, float (&c)[N], float (&s)[N]) {
-  long long p = a.pos ? (long long)a.pos[row] : row % a.T;
+// The packed sequence whose slot holds the row (uniform): the last one that starts no later,
+// found by the wave's lanes in steps of 64 to one.
+__device__ __forceinline__ int sequence_of(const attn::Batch& b, int row) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0;
+  for (int n = b.N; n > 1;) {
+    const int step = (n + 63) / 64, at = lane * step;
+    const int starts = __popcll(__ballot(at < n && b.off[lo + (at < n ? at : 0)] <= row));
+    const int skip = starts > 1 ? (starts - 1) * step : 0;
+    lo += skip;
+    n = n - skip < step ? n - skip : step;
+  }
+  return lo;
+}
+// Whether the row (uniform) is a token, and its position, clamped into the table: pos[row],
+// or its place in its sequence.
+__device__ __forceinline__ bool token(const RopeArgs& a, long long row, long long& p) {
+  long long at;
+  bool is = true;
+  if (a.batch) {
+    const int seq = a.b.off ? sequence_of(a.b, (int)row) : (int)attn::over((unsigned)row, a.perT);
+    const attn::Seq s = attn::sequence(a.b, seq);
+    at = row - s.first;
+    is = at >= 0 && at < s.len;
+  } else {
+    at = a.pos ? 0 : row % a.T;
+  }
+  p = a.pos ? (long long)a.pos[row] : at;
   p = p < 0 ? 0 : (p >= a.table_rows ? a.table_rows - 1 : p);
+  return is;
+}
+// zeros in the row's outputs
+template <int ROW>   // bytes of a head
+__device__ __forceinline__ void zero_row(const RopeArgs& a, long long row, int lane) {
+  for (int i = lane; i < a.H * (ROW / 16); i += 64) {
+    const int q = a.Hq * (ROW / 16);
+    unsigned char* o = i < q ? a.oq + row * a.ldoq + i * 16ll : a.ok + row * a.ldok + (i - q) * 16ll;
+    *reinterpret_cast<u32x4*>(o) = u32x4{0u, 0u, 0u, 0u};
+  }
+}
+
+// the lane's N angles at position p
+template <bool PAIRS, int N, int D>
+__device__ __forceinline__ void load_angles(const RopeArgs& a, long long p, int j, float (&c)[N], float (&s)[N]) {
   const f32x4* t = reinterpret_cast<const f32x4*>(a.table + p * D);
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) {   // two (cos, sin) pairs each
@@ -135,10 +177,15 @@ template <bool BF16, int D, bool PAIRS, bool NORM>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   constexpr int N = BF16 ? 8 : 4, L = D / 2 / N, E = BF16 ? 2 : 4, HPW = 64 / L;
   const int lane = threadIdx.x & 63, j = lane % L, hl = lane / L;
-  const long long row = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const long long row = (long long)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (row >= a.rows) return;
+  long long p;
+  if (!token(a, row, p)) {
+    zero_row<D * E>(a, row, lane);
+    return;
+  }
   float c[N], s[N];
-  load_angles<PAIRS, N, D>(a, row, j, c, s);
+  load_angles<PAIRS, N, D>(a, p, j, c, s);
   for (int h = hl; h < a.H; h += HPW) {
     const bool isq = h < a.Hq;
     const long long at = (long long)(isq ? h : h - a.Hq) * (D * E) + j * 16;
@@ -176,10 +223,15 @@ __global__ __launch_bounds__(kThreads) void rope_back_kernel(RopeArgs a) {
   constexpr int N = BF16 ? 8 : 4, L = D / 2 / N, E = BF16 ? 2 : 4, HPW = 64 / L;
   const int lane = threadIdx.x & 63, j = lane % L, hl = lane / L;
   float sum[2][2 * N] = {};
-  for (long long row = (long long)blockIdx.x * kWaves + (threadIdx.x >> 6); row < a.rows;
+  for (long long row = (long long)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); row < a.rows;
        row += (long long)gridDim.x * kWaves) {
+    long long p;
+    if (!token(a, row, p)) {
+      zero_row<D * E>(a, row, lane);
+      continue;
+    }
     float c[N], s[N];
-    load_angles<PAIRS, N, D>(a, row, j, c, s);
+    load_angles<PAIRS, N, D>(a, p, j, c, s);
     for (int h = hl; h < a.H; h += HPW) {
       const bool isq = h < a.Hq;
       const long long at = (long long)(isq ? h : h - a.Hq) * (D * E) + j * 16;
@@ -305,23 +357,33 @@ bool good(const void* p, int64_t ld, int64_t H, int64_t D, int64_t rows, dr_dtyp
   return p && aligned16(p) && ld >= H * D && ld % (dtype == DR_BF16 ? 8 : 4) == 0;
 }
 
-}  // namespace
-}  // namespace dr
+// The batch's layout; as it stands in b, without one a.batch stays false.
+dr_status set_batch(RopeArgs& a, const attn::Batch& b, int64_t N) {
+  if (N < 0 || b.T < 0) return DR_ERR_ARG;
+  if (N > 0x7fffffff || b.T > 0x7fffffff) return DR_ERR_UNSUPPORTED;
+  if (b.off ? N == 0 && b.rows > 0 : b.rows != N * b.T) return DR_ERR_ARG;
+  a.batch = b.off || b.len;
+  a.b = b;
+  a.b.N = (int)N;
+  a.perT = attn::divisor((unsigned)(b.T > 0 ? b.T : 1));
+  return DR_OK;
+}
 
-extern "C" dr_status dr_qk_norm_rope(const void* q, int64_t ldq, const void* k, int64_t ldk, int64_t rows, int64_t T, int Hq,
-                                     int Hkv, int64_t D, dr_dtype dtype, const float* wq, const float* wk, float eps,
-                                     const float* table, int64_t table_rows, const int32_t* pos, dr_rope_pairing pairing,
-                                     void* q_out, int64_t ldqo, void* k_out, int64_t ldko, void* stream) {
-  using namespace dr;
+// b, N: NULL without a batch's layout
+dr_status forward(const void* q, int64_t ldq, const void* k, int64_t ldk, int64_t rows, int64_t T, const attn::Batch* b,
+                  int64_t N, int Hq, int Hkv, int64_t D, dr_dtype dtype, const float* wq, const float* wk, float eps,
+                  const float* table, int64_t table_rows, const int32_t* pos, dr_rope_pairing pairing, void* q_out,
+                  int64_t ldqo, void* k_out, int64_t ldko, void* stream) {
   const dr_status st = check_sizes(rows, T, Hq, Hkv, D, dtype, wq, wk, eps, table, table_rows, pos);
   if (st != DR_OK) return st;
   if (pairing != DR_ROPE_HALVES && pairing != DR_ROPE_NEIGHBOURS) return DR_ERR_ARG;
   if (!good(q, ldq, Hq, D, rows, dtype) || !good(k, ldk, Hkv, D, rows, dtype) || !good(q_out, ldqo, Hq, D, rows, dtype) ||
       !good(k_out, ldko, Hkv, D, rows, dtype))
     return DR_ERR_ARG;
-  if (rows == 0) return DR_OK;
-  const int e = dtype == DR_BF16 ? 2 : 4;
   RopeArgs a = {};
+  const dr_status laid = b ? set_batch(a, *b, N) : DR_OK;
+  if (laid != DR_OK || rows == 0) return laid;
+  const int e = dtype == DR_BF16 ? 2 : 4;
   a.q = (const unsigned char*)q;
   a.k = (const unsigned char*)k;
   a.oq = (unsigned char*)q_out;
@@ -335,18 +397,11 @@ extern "C" dr_status dr_qk_norm_rope(const void* q, int64_t ldq, const void* k, 
   return launch_status();
 }
 
-extern "C" size_t dr_qk_norm_rope_workspace_size(int64_t rows, int64_t D) {
-  if (rows < 1 || D < 1) return 0;
-  return (size_t)dr::back_blocks(rows) * 2 * (size_t)D * sizeof(float);
-}
-
-extern "C" dr_status dr_qk_norm_rope_backward(const void* gq, int64_t ldgq, const void* gk, int64_t ldgk, const void* q,
-                                              int64_t ldq, const void* k, int64_t ldk, int64_t rows, int64_t T, int Hq,
-                                              int Hkv, int64_t D, dr_dtype dtype, const float* wq, const float* wk, float eps,
-                                              const float* table, int64_t table_rows, const int32_t* pos,
-                                              dr_rope_pairing pairing, void* dq, int64_t lddq, void* dk, int64_t lddk,
-                                              float* dwq, float* dwk, void* workspace, size_t ws_bytes, void* stream) {
-  using namespace dr;
+dr_status backward(const void* gq, int64_t ldgq, const void* gk, int64_t ldgk, const void* q, int64_t ldq, const void* k,
+                   int64_t ldk, int64_t rows, int64_t T, const attn::Batch* b, int64_t N, int Hq, int Hkv, int64_t D,
+                   dr_dtype dtype, const float* wq, const float* wk, float eps, const float* table, int64_t table_rows,
+                   const int32_t* pos, dr_rope_pairing pairing, void* dq, int64_t lddq, void* dk, int64_t lddk, float* dwq,
+                   float* dwk, void* workspace, size_t ws_bytes, void* stream) {
   const dr_status st = check_sizes(rows, T, Hq, Hkv, D, dtype, wq, wk, eps, table, table_rows, pos);
   if (st != DR_OK) return st;
   if (pairing != DR_ROPE_HALVES && pairing != DR_ROPE_NEIGHBOURS) return DR_ERR_ARG;
@@ -355,10 +410,11 @@ extern "C" dr_status dr_qk_norm_rope_backward(const void* gq, int64_t ldgq, cons
       !good(dk, lddk, Hkv, D, rows, dtype))
     return DR_ERR_ARG;
   if (norm && (!good(q, ldq, Hq, D, rows, dtype) || !good(k, ldk, Hkv, D, rows, dtype) || !dwq || !dwk)) return DR_ERR_ARG;
-  if (rows == 0 && !norm) return DR_OK;
+  RopeArgs a = {};
+  const dr_status laid = b ? set_batch(a, *b, N) : DR_OK;
+  if (laid != DR_OK || (rows == 0 && !norm)) return laid;
   if (norm && rows > 0 && (!workspace || ws_bytes < dr_qk_norm_rope_workspace_size(rows, D))) return DR_ERR_WORKSPACE;
   const int e = dtype == DR_BF16 ? 2 : 4;
-  RopeArgs a = {};
   a.gq = (const unsigned char*)gq;
   a.gk = (const unsigned char*)gk;
   a.q = (const unsigned char*)q;
@@ -376,4 +432,51 @@ extern "C" dr_status dr_qk_norm_rope_backward(const void* gq, int64_t ldgq, cons
   if (norm)   // (no rows: writes zeros)
     rope_sum_kernel<<<(int)(2 * D / kSumCols), kSumThreads, 0, hs>>>(a.partial, blocks, (int)D, dwq, dwk);
   return launch_status();
+}
+
+}  // namespace
+}  // namespace dr
+
+extern "C" dr_status dr_qk_norm_rope(const void* q, int64_t ldq, const void* k, int64_t ldk, int64_t rows, int64_t T, int Hq,
+                                     int Hkv, int64_t D, dr_dtype dtype, const float* wq, const float* wk, float eps,
+                                     const float* table, int64_t table_rows, const int32_t* pos, dr_rope_pairing pairing,
+                                     void* q_out, int64_t ldqo, void* k_out, int64_t ldko, void* stream) {
+  return dr::forward(q, ldq, k, ldk, rows, T, nullptr, 0, Hq, Hkv, D, dtype, wq, wk, eps, table, table_rows, pos, pairing,
+                     q_out, ldqo, k_out, ldko, stream);
+}
+
+extern "C" dr_status dr_qk_norm_rope_batch(const void* q, int64_t ldq, const void* k, int64_t ldk, int64_t rows, int64_t N,
+                                           int64_t T, const int32_t* off, const int32_t* len, int Hq, int Hkv, int64_t D,
+                                           dr_dtype dtype, const float* wq, const float* wk, float eps, const float* table,
+                                           int64_t table_rows, const int32_t* pos, dr_rope_pairing pairing, void* q_out,
+                                           int64_t ldqo, void* k_out, int64_t ldko, void* stream) {
+  const dr::attn::Batch b = {off, len, rows, T, 0};
+  return dr::forward(q, ldq, k, ldk, rows, T > 0 ? T : 1, &b, N, Hq, Hkv, D, dtype, wq, wk, eps, table, table_rows, pos,
+                     pairing, q_out, ldqo, k_out, ldko, stream);
+}
+
+extern "C" size_t dr_qk_norm_rope_workspace_size(int64_t rows, int64_t D) {
+  if (rows < 1 || D < 1) return 0;
+  return (size_t)dr::back_blocks(rows) * 2 * (size_t)D * sizeof(float);
+}
+
+extern "C" dr_status dr_qk_norm_rope_backward(const void* gq, int64_t ldgq, const void* gk, int64_t ldgk, const void* q,
+                                              int64_t ldq, const void* k, int64_t ldk, int64_t rows, int64_t T, int Hq,
+                                              int Hkv, int64_t D, dr_dtype dtype, const float* wq, const float* wk, float eps,
+                                              const float* table, int64_t table_rows, const int32_t* pos,
+                                              dr_rope_pairing pairing, void* dq, int64_t lddq, void* dk, int64_t lddk,
+                                              float* dwq, float* dwk, void* workspace, size_t ws_bytes, void* stream) {
+  return dr::backward(gq, ldgq, gk, ldgk, q, ldq, k, ldk, rows, T, nullptr, 0, Hq, Hkv, D, dtype, wq, wk, eps, table,
+                      table_rows, pos, pairing, dq, lddq, dk, lddk, dwq, dwk, workspace, ws_bytes, stream);
+}
+
+extern "C" dr_status dr_qk_norm_rope_batch_backward(
+    const void* gq, int64_t ldgq, const void* gk, int64_t ldgk, const void* q, int64_t ldq, const void* k, int64_t ldk,
+    int64_t rows, int64_t N, int64_t T, const int32_t* off, const int32_t* len, int Hq, int Hkv, int64_t D, dr_dtype dtype,
+    const float* wq, const float* wk, float eps, const float* table, int64_t table_rows, const int32_t* pos,
+    dr_rope_pairing pairing, void* dq, int64_t lddq, void* dk, int64_t lddk, float* dwq, float* dwk, void* workspace,
+    size_t ws_bytes, void* stream) {
+  const dr::attn::Batch b = {off, len, rows, T, 0};
+  return dr::backward(gq, ldgq, gk, ldgk, q, ldq, k, ldk, rows, T > 0 ? T : 1, &b, N, Hq, Hkv, D, dtype, wq, wk, eps, table,
+                      table_rows, pos, pairing, dq, lddq, dk, lddk, dwq, dwk, workspace, ws_bytes, stream);
 }

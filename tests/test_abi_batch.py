@@ -143,3 +143,24 @@ def test_cross_entropy_leading_dimensions(lib, back):
     for ld, ok in [(1 << 24, True), (1 << 32, True), ((1 << 32) + 8, False)]:
         for name in ("ldh", "lddh", "lddw") if back else ("ldh",):
             assert xent(lib, back, ws=None, **{name: ld}) == (DR_ERR_WORKSPACE if ok else DR_ERR_ARG), (name, ld)
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_rope_batch(lib, back):
+    def call(**kw):
+        d = dict(rows=64, N=2, T=32, off=None, len=FAKE, pos=None, D=64, ldq=256, table=FAKE, ws=FAKE, wsb=1 << 30)
+        d.update(kw)
+        head = [FAKE, d["ldq"], FAKE, 128, d["rows"], d["N"], d["T"], d["off"], d["len"], 4, 2, d["D"], DR_BF16, FAKE, FAKE,
+                1e-6, d["table"], 16, d["pos"], 0, FAKE, 256, FAKE, 128]
+        if back:
+            return lib.dr_qk_norm_rope_batch_backward(FAKE, 256, FAKE, 128, *head, FAKE, FAKE, d["ws"], d["wsb"], None)
+        return lib.dr_qk_norm_rope_batch(*head, None)
+    for kw, want in [(dict(N=-1), DR_ERR_ARG), (dict(T=-1, pos=FAKE), DR_ERR_ARG), (dict(rows=63), DR_ERR_ARG),
+                     (dict(off=FAKE, N=0), DR_ERR_ARG), (dict(D=96), DR_ERR_UNSUPPORTED), (dict(ldq=248), DR_ERR_ARG),
+                     (dict(table=None), DR_ERR_ARG), (dict(off=FAKE, T=1 << 31), DR_ERR_UNSUPPORTED),
+                     (dict(off=FAKE, N=1 << 31), DR_ERR_UNSUPPORTED)]:
+        assert call(**kw) == want, kw
+    if back:
+        assert call(ws=None) == DR_ERR_WORKSPACE and call(wsb=8) == DR_ERR_WORKSPACE
+    else:
+        assert call(rows=0, N=0) == DR_OK and call(rows=0, N=2, T=0) == DR_OK

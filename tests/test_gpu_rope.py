@@ -138,3 +138,91 @@ def test_refusals():
     with pytest.raises(_lib.DrError) as e:
         api.qk_norm_rope(off, k, tab, pos=pos)
     assert e.value.status == _lib.DR_ERR_ARG
+
+
+def check_batch(dtype, D, norm, spans, rows, where, given_pos, bad, seed):
+    """Rows outside the spans are padding of bits `bad`: zeros come out there, nothing of them enters dwq and dwk, and the
+    tokens get what they get without any."""
+    q, k, gq, gk, wq, wk, pos = inputs(rows, 6, 2, D, dtype, False, seed)
+    if not norm:
+        wq = wk = None
+    tab = table_of(300, D)
+    live = torch.zeros(rows, dtype=torch.bool)
+    place = torch.zeros(rows, dtype=torch.int64)
+    for a, b in spans:
+        live[a:b] = True
+        place[a:b] = torch.arange(b - a)
+    if not given_pos:
+        pos = place.to(torch.int32).to(DEV)
+    whole = api.qk_norm_rope(q, k, tab, wq, wk, eps=1e-5, pos=pos)
+    for t in (q, k, gq, gk):
+        t[~live.to(DEV)] = bad
+    if where.get("shape"):
+        q, k, gq, gk = [t.view(*where["shape"], *t.shape[1:]) for t in (q, k, gq, gk)]
+    kw = dict(offsets=where.get("offsets"), lengths=where.get("lengths"), max_len=where.get("max_len"))
+    out = api.qk_norm_rope(q, k, tab, wq, wk, eps=1e-5, pos=pos if given_pos else None, **kw)
+    grads = api.qk_norm_rope_backward(gq, gk, q, k, tab, wq, wk, eps=1e-5, pos=pos if given_pos else None, **kw)
+    flat = lambda t: t.reshape(rows, -1, D).cpu()     # noqa: E731
+    for x, w, o, plain, g, dx, dw in ((q, wq, out[0], whole[0], gq, grads[0], grads[2]),
+                                      (k, wk, out[1], whole[1], gk, grads[1], grads[3])):
+        assert torch.equal(flat(o)[live], flat(plain)[live])
+        assert bool((flat(o)[~live] == 0).all()) and bool((flat(dx)[~live] == 0).all())
+        dx_ref, dw_ref = ref.norm_rope_back(flat(g)[live], flat(x)[live], w, 1e-5, tab, pos.cpu()[live], False)
+        assert rel(flat(dx)[live], dx_ref) <= 2 * TOL[dtype]
+        if norm:
+            assert rel(dw, dw_ref) <= TOL_DW
+    again = api.qk_norm_rope_backward(gq, gk, q, k, tab, wq, wk, eps=1e-5, pos=pos if given_pos else None, **kw)
+    assert all(a is b or torch.equal(a, b) for a, b in zip(grads, again))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("norm,given_pos", [(True, False), (True, True), (False, False)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), 7.0])
+def test_padded_batch(dtype, D, norm, given_pos, bad):
+    for N, T in ((5, 33), (1, 1), (900, 7), (4, 1)):
+        lens = [(0, 1, T, T // 2, T - 1)[i % 5] for i in range(N)]
+        lengths = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        check_batch(dtype, D, norm, ref.spans_of(None, lens, N, T), N * T, dict(shape=(N, T), lengths=lengths), given_pos, bad, 21)
+    lens = [-3, 1 << 30]                             # out of range: none, all
+    check_batch(dtype, D, norm, [(9, 18)], 18, dict(shape=(2, 9), lengths=torch.tensor(lens, dtype=torch.int32, device=DEV)),
+                given_pos, bad, 22)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N", [1, 2, 63, 64, 65, 130, 5000])
+@pytest.mark.parametrize("given_pos", [False, True])
+def test_packed_batch(dtype, N, given_pos):
+    """Slots of 0 to 12 rows, lengths inside them, the most tokens of one below the longest slot, rows after the last."""
+    slots = [(i * 7 + 3) % 13 for i in range(N)]
+    off = [0]
+    for n in slots:
+        off.append(off[-1] + n)
+    lens, most, rows = [(i * 5) % 14 for i in range(N)], 11, off[-1] + 6
+    offsets, lengths = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (off, lens))
+    spans = [(a, min(b, a + n, a + most)) for a, b, n in zip(off, off[1:], lens)]
+    check_batch(dtype, 64, True, spans, rows, dict(offsets=offsets, lengths=lengths, max_len=most), given_pos, float("nan"), 23)
+    spans = [(a, min(b, a + most)) for a, b in zip(off, off[1:])]
+    check_batch(dtype, 64, True, spans, rows, dict(offsets=offsets, max_len=most), given_pos, float("nan"), 24)
+    wild = offsets.clone()
+    wild[0], wild[-1] = -5, 1 << 30                  # out of range: the first row, the last
+    spans[-1] = (off[-2], min(rows, off[-2] + most))
+    check_batch(dtype, 64, True, spans, rows, dict(offsets=wild, max_len=most), given_pos, float("nan"), 25)
+
+
+def test_batch_without_tokens_and_refusals():
+    q, k, gq, gk, wq, wk, pos = inputs(6, 2, 1, 64, torch.bfloat16, False, 26)
+    tab = table_of(300, 64)
+    none = torch.zeros(2, dtype=torch.int32, device=DEV)
+    four = [t.view(2, 3, -1, 64) for t in (q, k, gq, gk)]
+    out = (*api.qk_norm_rope(*four[:2], tab, wq, wk, lengths=none),
+           *api.qk_norm_rope_backward(*four[2:], *four[:2], tab, wq, wk, lengths=none))
+    assert all(float(t.float().abs().max()) == 0 for t in out)
+    e = q[:0], k[:0]
+    assert all(t.numel() == 0 for t in api.qk_norm_rope(*e, tab, wq, wk, offsets=none[:1], max_len=0))
+    for kw in (dict(offsets=none), dict(offsets=none.long(), max_len=3), dict(lengths=none), dict(lengths=none, max_len=4),
+               dict(lengths=none.float(), max_len=3), dict(lengths=none[:1], max_len=3)):
+        with pytest.raises(ValueError):
+            api.qk_norm_rope(q, k, tab, wq, wk, **kw)
+        with pytest.raises(ValueError):
+            api.qk_norm_rope_backward(gq, gk, q, k, tab, wq, wk, **kw)

@@ -16,6 +16,9 @@
 // one bf16 head) is read once per row and not once per head.  bf16, D = 128: 16384 rows
 // of 40 heads out of the fused projection, rotated only, 64 us (5.2 TB/s, where a copy
 // reaches 4.9); 36864 rows of 24 heads with norms 79 us, their gradients 134 us (680 MB).
+// Of a batch with padding (72 slots of 512 of those rows, 128 to 512 tokens in each: 0.62 are
+// tokens) 77 and 120 us in calls of their own, where all rows take 86 and 135: padding rows
+// are written, not read.  The same tokens packed, with offsets, 57 and 87.
 #include "attn.h"   // the batch's rows
 
 namespace dr {
@@ -121,12 +124,14 @@ __device__ __forceinline__ int sequence_of(const attn::Batch& b, int row) {
   }
   return lo;
 }
-// Whether the row (uniform) is a token, and its position, clamped into the table: pos[row],
-// or its place in its sequence.
+// Whether the row is a token, and its position, clamped into the table: pos[row], or its
+// place in its sequence.  BATCH: the row is uniform; the kernels without it keep theirs (with
+// one kernel for both: rope_train 225 us, 223 without).
+template <bool BATCH>
 __device__ __forceinline__ bool token(const RopeArgs& a, long long row, long long& p) {
   long long at;
   bool is = true;
-  if (a.batch) {
+  if constexpr (BATCH) {
     const int seq = a.b.off ? sequence_of(a.b, (int)row) : (int)attn::over((unsigned)row, a.perT);
     const attn::Seq s = attn::sequence(a.b, seq);
     at = row - s.first;
@@ -137,6 +142,12 @@ __device__ __forceinline__ bool token(const RopeArgs& a, long long row, long lon
   p = a.pos ? (long long)a.pos[row] : at;
   p = p < 0 ? 0 : (p >= a.table_rows ? a.table_rows - 1 : p);
   return is;
+}
+// this wave's number: uniform where rows are looked up
+template <bool BATCH>
+__device__ __forceinline__ int wave() {
+  const int w = threadIdx.x >> 6;
+  return BATCH ? __builtin_amdgcn_readfirstlane(w) : w;
 }
 // zeros in the row's outputs
 template <int ROW>   // bytes of a head
@@ -173,14 +184,14 @@ __device__ __forceinline__ void load_weight(const float* w, int col, float (&v)[
   }
 }
 
-template <bool BF16, int D, bool PAIRS, bool NORM>
+template <bool BF16, int D, bool PAIRS, bool NORM, bool BATCH>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   constexpr int N = BF16 ? 8 : 4, L = D / 2 / N, E = BF16 ? 2 : 4, HPW = 64 / L;
   const int lane = threadIdx.x & 63, j = lane % L, hl = lane / L;
-  const long long row = (long long)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long row = (long long)blockIdx.x * kWaves + wave<BATCH>();
   if (row >= a.rows) return;
   long long p;
-  if (!token(a, row, p)) {
+  if (!token<BATCH>(a, row, p)) {
     zero_row<D * E>(a, row, lane);
     return;
   }
@@ -218,15 +229,15 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
 // A block takes rows in strides of the grid; a lane keeps its columns' sums of
 // dy * x * r for queries and for keys, which the block joins in LDS in a fixed
 // order and leaves as one partial row.
-template <bool BF16, int D, bool PAIRS, bool NORM>
+template <bool BF16, int D, bool PAIRS, bool NORM, bool BATCH>
 __global__ __launch_bounds__(kThreads) void rope_back_kernel(RopeArgs a) {
   constexpr int N = BF16 ? 8 : 4, L = D / 2 / N, E = BF16 ? 2 : 4, HPW = 64 / L;
   const int lane = threadIdx.x & 63, j = lane % L, hl = lane / L;
   float sum[2][2 * N] = {};
-  for (long long row = (long long)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); row < a.rows;
+  for (long long row = (long long)blockIdx.x * kWaves + wave<BATCH>(); row < a.rows;
        row += (long long)gridDim.x * kWaves) {
     long long p;
-    if (!token(a, row, p)) {
+    if (!token<BATCH>(a, row, p)) {
       zero_row<D * E>(a, row, lane);
       continue;
     }
@@ -316,16 +327,21 @@ __global__ __launch_bounds__(kSumThreads) void rope_sum_kernel(const float* part
   else dwk[col - D] = v;
 }
 
-template <bool BACK, bool BF16, int D>
+template <bool BACK, bool BF16, int D, bool BATCH>
 void launch(const RopeArgs& a, bool pairs, bool norm, int blocks, hipStream_t hs) {
   auto go = [&](auto kern) { kern<<<blocks, kThreads, 0, hs>>>(a); };
   if constexpr (BACK) {
-    if (pairs) norm ? go(rope_back_kernel<BF16, D, true, true>) : go(rope_back_kernel<BF16, D, true, false>);
-    else norm ? go(rope_back_kernel<BF16, D, false, true>) : go(rope_back_kernel<BF16, D, false, false>);
+    if (pairs) norm ? go(rope_back_kernel<BF16, D, true, true, BATCH>) : go(rope_back_kernel<BF16, D, true, false, BATCH>);
+    else norm ? go(rope_back_kernel<BF16, D, false, true, BATCH>) : go(rope_back_kernel<BF16, D, false, false, BATCH>);
   } else {
-    if (pairs) norm ? go(rope_kernel<BF16, D, true, true>) : go(rope_kernel<BF16, D, true, false>);
-    else norm ? go(rope_kernel<BF16, D, false, true>) : go(rope_kernel<BF16, D, false, false>);
+    if (pairs) norm ? go(rope_kernel<BF16, D, true, true, BATCH>) : go(rope_kernel<BF16, D, true, false, BATCH>);
+    else norm ? go(rope_kernel<BF16, D, false, true, BATCH>) : go(rope_kernel<BF16, D, false, false, BATCH>);
   }
+}
+template <bool BACK, bool BF16, int D>
+void launch(const RopeArgs& a, bool pairs, bool norm, int blocks, hipStream_t hs) {
+  if (a.batch) launch<BACK, BF16, D, true>(a, pairs, norm, blocks, hs);
+  else launch<BACK, BF16, D, false>(a, pairs, norm, blocks, hs);
 }
 template <bool BACK>
 void launch(const RopeArgs& a, bool bf16, int64_t D, bool pairs, bool norm, int blocks, hipStream_t hs) {

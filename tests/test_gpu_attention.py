@@ -350,3 +350,51 @@ def test_nan_reaches_the_statistics_it_belongs_to(D, Hq, Hkv):
         o, lse = api.attention(x if which is q else q, x if which is k else k, v, **where)
         assert bool(torch.isnan(lse[:, bad]).all()) and bool(torch.isnan(o[bad].float()).all())
         assert torch.equal(lse[:, ~bad], base[:, ~bad])
+
+
+def bounds(q, k, v, g, spans, scale):
+    """What each row of o, dq, dk, dv of each head may be off by, in norm, given the roundings to bf16 (2^-8 of a value each):
+    P, with sums of P and dS in fp32, dS, o in delta, and the outputs.  5 % more for fp32 arithmetic."""
+    q, k, v, g = (ref.d64(t) for t in (q, k, v, g))
+    rows, Hq, D = q.shape
+    G = Hq // k.shape[1]
+    out = [torch.zeros(rows, n, dtype=torch.float64) for n in (Hq, Hq, k.shape[1], k.shape[1])]
+    for a, b in spans:
+        hide = torch.ones(b - a, b - a, dtype=torch.bool).triu(1)
+        for h in range(Hq if b > a else 0):
+            Q, K, V, dO = q[a:b, h], k[a:b, h // G], v[a:b, h // G], g[a:b, h]
+            P = torch.softmax((scale * Q @ K.t()).masked_fill(hide, -float("inf")), -1)
+            O = P @ V
+            weight = P @ V.norm(dim=1) + O.norm(dim=1)           # what o's error may be 2^-8 of
+            off = dO.norm(dim=1) * weight                        # delta's
+            dS = (P * (dO @ V.t() - (dO * O).sum(-1, keepdim=True))).abs()
+            out[0][a:b, h] = weight
+            out[1][a:b, h] = scale * (dS @ K.norm(dim=1) + off * (P @ K).norm(dim=1))
+            out[2][a:b, h // G] += scale * (dS.t() @ Q.norm(dim=1) + P.t() @ (off * Q.norm(dim=1)))
+            out[3][a:b, h // G] += P.t() @ dO.norm(dim=1)
+    o, lse, dq, dk, dv = ref.attention(q, k, v, spans, scale, g)
+    for x, t in zip(out[1:], (dq, dk, dv)):
+        x += t.norm(dim=-1)
+    return [1.05 * U_BF16 * x for x in out], (o, dq, dk, dv)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("lens,Hq,Hkv", [(EDGES, 4, 2), ([700, 650, 300, 5], 8, 8), ([700, 650, 300, 5], 8, 2), ([900, 70], 10, 2),
+                                         ([1100], 2, 1)])
+def test_rows_one_by_one(D, lens, Hq, Hkv):
+    """Every row of every head by itself, so that a few wrong values of a tile's edge show: tiles of 32 rows and 128, dk and
+    dv whole and in parts."""
+    off = [0]
+    for n in lens:
+        off.append(off[-1] + n)
+    offsets = torch.tensor(off, dtype=torch.int32, device=DEV)
+    q, k, v, g = make(off[-1], Hq, Hkv, D, True, 33)
+    where = dict(offsets=offsets, max_len=max(lens))
+    spans = ref.spans_of(off, None, len(lens), 0)
+    o, lse = api.attention(q, k, v, **where)
+    got = (o, *api.attention_backward(g, q, k, v, o, lse, **where))
+    limit, want = bounds(q, k, v, g, spans, D ** -0.5)
+    for x, y, m in zip(got, want, limit):
+        worst = ((ref.d64(x) - y).norm(dim=-1) / m).max()
+        print(f"{float(worst):.2f} of the bound")
+        assert float(worst) <= 1.0

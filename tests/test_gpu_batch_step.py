@@ -79,3 +79,32 @@ def test_step_matches_autograd():
     # the update of the output map: the mean gradient of the selected examples
     want = sum(grads[3][i].t() @ outs[i] for i in idx[0].tolist()) / 2
     assert rel(updates[3], want) <= 2 * TOL
+
+
+def test_scores_and_selection_match_autograd():
+    """The scores against those of the fp64 gradients' sketches: a product of two sketches, each within TOL of its size.  The
+    selected examples are the best ones but for scores that this does not tell apart."""
+    import merged_batch_step as step
+    import oracle
+    n, m, T, d, V, k = 11, 4, 70, 128, 333, 4
+    w = step.make_block(d, Hq=4, Hkv=2, D=64, V=V, T=T, device=DEV)
+    x, lens, target = step.make_batch(n + m, T, d, V, DEV)
+    _, outs, grads = autograd_pairs(w, x, lens, target)
+    for i in range(n + m):
+        x[i, int(lens[i]):] = 7.0
+    _, pairs = step.forward_backward(w, x, lens, target)
+    s, idx, _, info = step.select_and_update(w, pairs, lens, n, k)
+    torch.cuda.synchronize()
+    ins = [ref.d64(x)] * 3 + [outs]
+    S = oracle.sketch_ref([dict(x=a.numpy(), dy=dy.numpy(), p_in=ref.d64(p[0]).numpy(), p_out=ref.d64(p[1]).numpy())
+                           for a, dy, p in zip(ins, grads, w["p"])], lens.cpu().numpy())
+    want = torch.from_numpy(oracle.gram_ref(S[:n], S[n:])[1][0])
+    size = torch.from_numpy(S[:n]).norm(dim=1) * float(torch.from_numpy(S[n:]).mean(0).norm())
+    err = (ref.d64(s[0]) - want).abs()
+    print(f"scores within {float((err / size).max()):.2e} of the sketches' sizes, which differ from 0 by "
+          f"{float((want.abs() / size).mean()):.2e} on average")
+    assert bool((err <= 2 * TOL * size).all())
+    got, best = sorted(idx[0].tolist()), want.topk(k).values[-1]
+    assert int(info[0]) == 0 and len(set(got)) == k
+    assert all(float(want[i]) >= float(best) - 4 * TOL * float(size.max()) for i in got)
+    assert got == sorted(ref.d64(s[0]).topk(k).indices.tolist())

@@ -921,19 +921,23 @@ int64_t piece_of(int64_t M, int64_t V) {
 bool use_strips(int64_t M, int64_t rows, int64_t cols, int64_t splits = 1) {
   return M <= kStrip || tiles_of(rows) * tiles_of(cols) * splits < kCUs / 2;
 }
+int strips_of(int64_t n) { return (int)((n + kStrip - 1) / kStrip); }
 // The logits' products (M tokens, n entries) also where there are few steps, and most of a
 // tile's time is what its one workgroup a CU does before and after them.  (8192 tokens,
 // 32768 entries: D = 64 forward 168 us in tiles and 124 in strips, backward 584 and 568; D
 // = 128 190 and 151, 628 and 629; D = 256 233 and 203, 752 and 778.)
-// Of many steps only below a third of the CUs, since a CU's DMA bounds strips: 256 tokens,
-// D = 4096, 32000 entries (125 tiles) 118 us in tiles and 158 in strips, 20000 (79) 97 and
-// 108; 2048 tokens, 2500 entries (80) 103 and 87; but 1000 of which 600 count, D = 2048,
-// 6000 entries (96) 59 and 40.
+// Of many steps (above 512 dimensions) and few tokens only up to 9/8 strips a CU: the strips
+// of one panel of W run on different XCDs, each of which reads it.  Forward, strips and tiles,
+// us, D = 2048 | 4096: 256 tokens by 16344 entries (256 strips) 49 and 57 | 80 and 96, by 20440
+// (320) 67 and 57 | 109 and 96; 512 by 8152 (256) 45 and 59 | 81 and 99, by 10200 (320) 62 and
+// 58 | 110 and 99; 700 by 6616 (286) 54 and 59 | 97 and 100, by 10712 (462) 68 and 60 | 130 and
+// 102.  Above 768 tokens, whose W is smaller for as many strips, as otherwise: 1000 by 7900
+// (496 strips, 124 tiles) 59 and 60 | 105 and 104, 2048 by 2800 (352, 88) 51 and 60 | 86 and
+// 104; and at D = 512: 256 by 20440 24 and 27, by 32216 (126 tiles) 31 and 28.
 bool logit_strips(int64_t M, int64_t n, int64_t D) {
-  if (D > 40 * kCols) return M <= kStrip || tiles_of(M) * tiles_of(n) < kCUs / 3;
+  if (D > 512 && M > kStrip && M <= 768) return strips_of(M) * tiles_of(n) <= kCUs + kCUs / 8;
   return use_strips(M, M, n) || D < 256;
 }
-int strips_of(int64_t n) { return (int)((n + kStrip - 1) / kStrip); }
 // Strips of 64 x 64 where those of 64 x 256 would leave CUs idle: a CU's DMA brings
 // 40 KB of operands a step of 64 indices in 0.6 us, however few workgroups there are.
 // (248 tokens, 531 entries, D = 2256: forward 31 us with 256 columns and 18 with 64,

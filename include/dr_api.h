@@ -455,7 +455,8 @@ size_t dr_score_workspace_size(const dr_layer* layers, int num_layers, int64_t n
  * its position, in one pass:
  *   y = x * (mean(x^2) + eps)^(-1/2) * w   over the head's D values
  *   out = y with its D/2 pairs turned by the angles of the row's position.
- *   q [rows][ldq], k [rows][ldk]; Hq >= 1, Hkv >= 0 heads; D in {64, 128}
+ *   q [rows][ldq], k [rows][ldk]; Hq >= 1, Hkv >= 0 heads, 65536 at most of
+ *             either (else DR_ERR_ARG); D in {64, 128}
  *             (else DR_ERR_UNSUPPORTED); dtype DR_F32 or DR_BF16 (inputs and
  *             outputs share it; arithmetic in fp32, one rounding at the end).
  *   wq, wk    fp32 [D] norm weights, or both NULL: rotation only.
@@ -532,7 +533,7 @@ dr_status dr_qk_norm_rope_batch_backward(const void* gq, int64_t ldgq, const voi
  * A NaN or infinity in a sequence's tokens reaches that sequence's rows only,
  * some before it among them (a masked weight is 0, and 0 times it is NaN).
  * Requirements (else DR_ERR_ARG): 0 < scale; ld >= H * D, multiples of 8, at
- * most 2^24; tensors 16-byte aligned.  rows < 2^31,
+ * most 2^24; tensors 16-byte aligned.  rows, N and T < 2^31,
  * N * ceil(T / 128) < 2^30, Hq <= 65536 (else DR_ERR_UNSUPPORTED).
  * ------------------------------------------------------------------------- */
 dr_status dr_attention(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
@@ -580,7 +581,9 @@ dr_status dr_cross_entropy(const void* h, int64_t ldh, const void* W, int64_t ld
  * with z recomputed and dz kept for a piece of the vocabulary at a time, in
  * bf16 and without the significand of g_i, which is applied to dh in fp32 and,
  * relative to the first token's, to a bf16 copy of h for dW (exact where all g_i
- * are alike; where it is not, 1 - softmax(z_i)[target_i] goes the same way).  Tokens without a loss get dh = 0 and add nothing to dW.
+ * are alike; where it is not, 1 - softmax(z_i)[target_i] goes the same way).  (So
+ * the bits of dW's rounding, not its size, depend on which token comes first.)
+ * Tokens without a loss get dh = 0 and add nothing to dW.
  *   lse       fp32 [M] of the forward call; g fp32 [M] (e.g. 1 / the example's
  *             number of tokens, for its mean loss).
  *   dh bf16 [M][lddh] or NULL; dW bf16 [V][lddw] or NULL (not wanted).

@@ -412,6 +412,11 @@ def dr_score_exact(layers, n, m, T, lengths, method, s, workspace=None, stream=N
 # the merged batch's forward and backward operators
 # ---------------------------------------------------------------------------
 
+# Like every call here these are not part of torch's autograd: outputs carry no
+# gradient function, whatever the inputs require, and the `_backward` calls are
+# the gradients for a caller's own autograd function.  Targets, positions,
+# offsets and lengths are int32.
+#
 # Small calls are bound by the host: these checks take a microsecond each, an
 # allocation with empty_like 1.2 us (2.3 with torch.empty), the call and its
 # launch 4.3; outputs that a convenience has just allocated are not checked again.

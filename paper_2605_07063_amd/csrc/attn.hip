@@ -15,10 +15,10 @@
 // With D = 128 a SIMD holds two waves (204 registers), with D = 64 four; MFMA and
 // softmax are about even (16 products and 128 VALU instructions, a quarter of them
 // exponentials, for 32 rows by 64 keys of D = 64) and wait for each other.  32 query
-// heads of 8 key heads, forward: 16 sequences of 1024, D = 128, 172 us (0.80 PFLOP/s;
-// MFMA busy 0.39, VALU 0.40); 4 of 4096 599 us (0.92; MFMA busy 0.57 at the 1.55 GHz
-// that power leaves); the same with D = 64 312 us (0.88; VALU busy 0.78); 72 examples of
-// 128 to 512 tokens, D = 64, 90 us, of which Q, K, V and O of HBM take 59.  Slower:
+// heads of 8 key heads, forward: 16 sequences of 1024, D = 128, 176 us (0.78 PFLOP/s;
+// MFMA busy 0.39, VALU 0.41); 4 of 4096 550 us (1.00; MFMA busy 0.57 at the 1.58 GHz
+// that power leaves); the same with D = 64 323 us (0.85; VALU busy 0.78); 72 examples of
+// 128 to 512 tokens, D = 64, 93 us, of which Q, K, V and O of HBM take 59.  Slower:
 // 64 rows a wave (D = 128 one wave a SIMD, +36 %; D = 64 +3 %), the values of a step beside
 // the next one's scores (+11 to +14 %), half a step's scores beside the other half's
 // weights (+15 to +23 %), raised priority around the products (no change).

@@ -16,9 +16,9 @@
 // Bound by the MFMA and the VALU work around it, which wait for each other in the
 // two waves of a SIMD that the registers allow (222 and 252 of 256 with D = 128).
 // Full sequences of 4096, 32 query heads of 8 key heads, D = 128, four of them: dq
-// 0.86 ms and dkv 1.16 (0.96 and 0.95 PFLOP/s; MFMA busy 0.57 and 0.55 at the 1.6 and
-// 1.7 GHz that power leaves), 16 of 1024: 0.31 and 0.37 ms, MFMA busy 0.37 and 0.48.
-// D = 64: 72 examples of 128 to 512 tokens 0.14 and 0.12 ms.  Slower: keys in pairs of
+// 0.81 ms and dkv 1.11 (1.02 and 0.99 PFLOP/s; MFMA busy 0.57 and 0.55 at the 1.6 and
+// 1.7 GHz that power leaves), 16 of 1024: 0.32 and 0.35 ms, MFMA busy 0.38 and 0.48.
+// D = 64: 72 examples of 128 to 512 tokens 0.15 and 0.13 ms.  Slower: keys in pairs of
 // waves that share P through LDS (1.60 ms instead of 1.18), 64 keys a wave (spills
 // with D = 128; 1.09 ms and 0.93 with D = 64), eight waves a workgroup.
 #include "attn.h"
@@ -499,7 +499,11 @@ namespace {
 // workgroups leave CUs idle at the end.)  None where the longest workgroup's steps are
 // few beside the number of workgroups, whose sums would cost more than that saves: 64
 // examples of 331 tokens (384 workgroups of at most 18 steps; 6 / 2 heads of 128) 109
-// us whole and 145 in three parts, 12 of 477 (192 of 24; 12 / 4 heads) 105 and 90.
+// us whole and 145 in three parts, 12 of 477 (192 of 24; 12 / 4 heads) 105 and 90.  Over
+// 240 shapes of 60 to 576 workgroups of 2 to 256 steps (D = 64, 128; 1 to 8 query heads a
+// key head; 100 to 2000 tokens) the parts' time over the whole's is 1.10 to 1.72 where 9
+// steps are 0.13 to 0.5 of the workgroups and there are steps to deal, 0.91 to 1.10 between
+// 0.8 and 1.25, 0.65 to 0.99 from 1.4 to 4, and down to 0.26 above.
 int most_parts(int64_t groups) {
   const int64_t p = (639 + groups) / groups;
   return (int)(p < 8 ? p : 8);

@@ -74,7 +74,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(const int* target, i
 // target's entry the power of two itself.  Errors against fp64, where rounding the
 // outputs alone makes 1.66e-3 and rounding g dz made 2.1e-3 to 2.3e-3: one g for all, dh
 // and dW 1.7e-3 to 1.8e-3; g of their own, dh 1.7e-3, dW 2.3e-3 to 2.4e-3 (2120 tokens,
-// 154 entries: with 1 - p left in dz dh 1.95e-3, dW 2.57e-3).
+// 154 entries: with 1 - p left in dz dh 1.95e-3, dW 2.57e-3), so that dW, which then takes
+// the rounding of h in place of that of dz, gains nothing, and dh does.
 __device__ __forceinline__ float significand(float g) {
   const unsigned u = __float_as_uint(g), e = u >> 23 & 0xff;
   return e == 0 || e == 255 ? 1.f : __uint_as_float((u & 0x7fffff) | 0x3f800000);
@@ -102,8 +103,11 @@ struct GatherArgs {
   const float* row_lse;
   float* rest;           // [M]: what of a token's dz, beside the significand, goes by way of h
 };
-// 1 - p of row src's target, by the whole workgroup; 1 where that is nearly or less than
-// nothing (p from this dot product and from the tiles' then differ by 2^-13 of it at most)
+// 1 - p of row src's target, by the whole workgroup; 1 where that is less than 2^-7.  This p
+// and the one that dz is formed from differ by fp32's roundings of the logit and of lse, about
+// 2^-24 of their size: by 2^-20 for an lse of 12, 2^-13 of 1 - p at most, and by more in
+// proportion for larger ones.  The target's entry of dz is the power of two only up to that;
+// what divides dz multiplies dh and h again, so nothing else rests on it.
 __device__ __forceinline__ float rest_of(const GatherArgs& a, long long src) {
   __shared__ float part[4];
   const unsigned char *h = a.h + src * a.ldh, *w = a.W + (long long)a.target[src] * a.ldw;
@@ -492,8 +496,8 @@ __device__ __forceinline__ u32x4 pair_bf16(f32x4 a, f32x4 b) {
 }
 
 // Logits of 256 tokens by 256 entries: their statistics (DZ = false), or dz.  Bound by
-// MFMA: 8192 tokens, 128000 entries, D = 4096 in 6.5 ms (1.32 PFLOP/s; MFMA busy 0.60 at
-// 2.06 GHz), dz of a quarter of the entries in 1.8 ms; of a tile's 106 us 11 are its
+// MFMA: 8192 tokens, 128000 entries, D = 4096 in 6.6 ms (1.30 PFLOP/s; MFMA busy 0.60 at
+// 2.05 GHz), dz of 32768 of the entries in 1.85 ms (1.19); of a tile's 106 us 11 are its
 // epilogue (54 of D = 2048).  Slower: 256 workgroups that take tile after tile, with the
 // next one's first steps on their way meanwhile (111 us a tile, 58 of D = 2048).
 template <bool DZ>
@@ -533,7 +537,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 }
 
 // sums of dh: += dz W over a part of the piece's vocabulary entries (8192 tokens,
-// 32768 entries, D = 4096: 1.7 ms, 1.28 PFLOP/s)
+// 32768 entries, D = 4096: 1.74 ms, 1.26 PFLOP/s)
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void dh_kernel(Args a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kTileRing];
   const int count = *a.count, ta = (count + kT - 1) / kT, splits = splits_now(a, count, kT);
@@ -588,7 +592,7 @@ __global__ __launch_bounds__(256) void dw_store_kernel(Args a) {
   store4(a.dW + (a.v0 + b) * a.lddw + 2 * c, v * weight_scale(a));
 }
 
-// rows v0 .. v1 - 1 of dW = dz^T h (the same sizes: 1.64 ms, 1.34 PFLOP/s)
+// rows v0 .. v1 - 1 of dW = dz^T h (the same sizes: 1.69 ms, 1.30 PFLOP/s)
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void dw_kernel(Args a) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kTileRing];
   const int count = *a.count;
@@ -619,7 +623,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
 // idle.  Two workgroups share a CU (four of 64 columns), each wave takes 64 columns (32
 // by 32), and the operands go through two stages of 40 KB (16 KB).  For few tokens bound
 // by reading W, or writing dW: 48 tokens, 128000 entries, D = 4096 (1.05 GB): statistics
-// 175 us (6.0 TB/s), dz 179, dh 230, dW 250 to 300.
+// 175 us (6.0 TB/s), dz 180, dh 232, dW 225 to 283.
 constexpr int kStrip = 64;
 constexpr int kStripB = kStrip * kCols * 2;
 

@@ -226,3 +226,31 @@ def test_batch_without_tokens_and_refusals():
             api.qk_norm_rope(q, k, tab, wq, wk, **kw)
         with pytest.raises(ValueError):
             api.qk_norm_rope_backward(gq, gk, q, k, tab, wq, wk, **kw)
+
+
+def test_side_stream_and_graph():
+    """The same bits on another stream, and from replays of a captured graph, with lengths and without."""
+    q, k, gq, gk, wq, wk, pos = inputs(260, 4, 2, 64, torch.bfloat16, True, 27)
+    tab = table_of(300, 64)
+    lengths = torch.tensor([0, 64, 65, 20], dtype=torch.int32, device=DEV)
+    for kw in (dict(), dict(lengths=lengths, max_len=65)):
+        want = (*api.qk_norm_rope(q, k, tab, wq, wk, pos=pos, **kw), *api.qk_norm_rope_backward(gq, gk, q, k, tab, wq, wk, pos=pos, **kw))
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        got = (*api.qk_norm_rope(q, k, tab, wq, wk, pos=pos, stream=side, **kw),
+               *api.qk_norm_rope_backward(gq, gk, q, k, tab, wq, wk, pos=pos, stream=side, **kw))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        out = [torch.empty_like(t) for t in want]
+        ws = torch.empty(api.dr_qk_norm_rope_workspace_size(260, 64), dtype=torch.uint8, device=DEV)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            api.dr_qk_norm_rope(q, k, tab, wq, wk, 1e-6, pos, False, *out[:2], **kw)
+            api.dr_qk_norm_rope_backward(gq, gk, q, k, tab, wq, wk, 1e-6, pos, False, *out[2:], workspace=ws, **kw)
+        for _ in range(3):
+            [t.fill_(7) for t in out]
+            ws.fill_(255)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, out))

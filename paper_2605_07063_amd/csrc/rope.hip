@@ -373,7 +373,8 @@ bool good(const void* p, int64_t ld, int64_t H, int64_t D, int64_t rows, dr_dtyp
   return p && aligned16(p) && ld >= H * D && ld % (dtype == DR_BF16 ? 8 : 4) == 0;
 }
 
-// The batch's layout; as it stands in b, without one a.batch stays false.
+// Takes the layout of b with its N sequences.  Without offsets and lengths every row is a
+// token, and the kernels without a lookup run.
 dr_status set_batch(RopeArgs& a, const attn::Batch& b, int64_t N) {
   if (N < 0 || b.T < 0) return DR_ERR_ARG;
   if (N > 0x7fffffff || b.T > 0x7fffffff) return DR_ERR_UNSUPPORTED;
